@@ -124,7 +124,7 @@ template <> struct Eight<Half> {
             w[p] = (w[p] & m) | (0xfbfffbffu & ~m);
         }
     }
-    // into range (NaN becomes `low`); the largest
+    // into range (NaN becomes `low`, a signalling one a quiet one); the largest of the numbers
     __device__ float settle()
     {
 #pragma unroll
@@ -368,8 +368,9 @@ __global__ __launch_bounds__(THREADS) void select_piece_kernel(const SelectArgs 
         for (int j = 0; j < 8; ++j) e[j] = exp_of<T>(v[u].minus(j, most));
         s += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
     }
-    if (most <= low + 200.f) {
-        // what is held as `low` would count among values so near to it: the sum once more, of what is there
+    if (most <= low + 200.f || s != s) {
+        // What is held as `low` would count among values so near to it; and a signalling NaN among fp16 logits, which one
+        // maximum makes a quiet one instead of `low`, is in the sum: the sum once more, of what is there.
         s = 0.0;
 #pragma unroll 1
         for (int u = 0; u < U; ++u) {
