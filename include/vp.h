@@ -366,9 +366,10 @@ vp_status vp_add_norm(const void *x, int64_t x_stride, const void *residual, int
                       const void *weight, int32_t weight_type, int64_t n, int32_t d, float eps, void *sum, void *norm,
                       int32_t norm_type, uint8_t *q, float *scales, float *rstd, void *hip_stream);
 
-/* The gradient of (sum, norm) with respect to x (the same for residual) and weight, from vp_add_norm's s and rstd:
- *   dx = rstd * weight * dnorm - s * rstd^3 * mean(weight * dnorm * s) + dsum     (rounded once)
- *   dweight = sum over rows of dnorm * s * rstd                                   (fp32, in a fixed order)
+/* The gradient of (sum, norm) with respect to x (the same for residual) and weight, from vp_add_norm's s and rstd; with
+ * h = s * rstd
+ *   dx = rstd * (weight * dnorm - h * mean(weight * dnorm * h)) + dsum     (rounded once)
+ *   dweight = sum over rows of dnorm * h                                   (fp32, in a fixed order)
  *   dnorm, s, dsum  device, type [n, d]; dsum may be NULL (zero);  dx  device, type [n, d];  dweight  device, fp32 [d]
  *   workspace       device, 256-byte aligned, >= vp_add_norm_grad_workspace_bytes(n, d) */
 size_t vp_add_norm_grad_workspace_bytes(int64_t n, int32_t d);

@@ -144,7 +144,8 @@ __global__ __launch_bounds__(64 * waves_of(W)) void add_norm_kernel(const NormAr
 }
 
 // ---------------------------------------------------------------- gradient
-//   dx = rstd * w * dnorm - s * rstd^3 * mean(w * dnorm * s) + dsum,   dweight = sum over rows of dnorm * s * rstd
+//   h = s * rstd,   dx = rstd * (w * dnorm - h * mean(w * dnorm * h)) + dsum,   dweight = sum over rows of dnorm * h
+// (h is of the order of one whatever the row's size; rstd^3 and w * dnorm * s leave 32 bits' range long before rstd does)
 // A workgroup takes every so many rows (W wavefronts to each) and keeps its share of dweight in registers; what its
 // wavefronts have of the same columns is joined in LDS, and a second kernel adds up the workgroups' in a fixed order.
 constexpr int GRAD_GROUPS = 1024;
@@ -191,15 +192,16 @@ __global__ __launch_bounds__(64 * waves_of(W)) void add_norm_grad_kernel(const N
         float dot = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            dw[j] += g[j] * f[j] * r;
+            f[j] *= r;
+            dw[j] += g[j] * f[j];
             g[j] *= w[j];
             dot += g[j] * f[j];
         }
-        const float k = r * r * r * per * row_sum_of<W>(dot, slot);
+        const float k = per * row_sum_of<W>(dot, slot);
         float o[8], e[8] = {};
         if (A.dsum) now.e.values(c, d, e);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = r * g[j] - f[j] * k + e[j];
+        for (int j = 0; j < 8; ++j) o[j] = r * (g[j] - f[j] * k) + e[j];
         if (row < A.n) put_within((T *)A.dx + (size_t)row * d, c, d, o, A.stream);
     }
     if (ROWS > 1) {

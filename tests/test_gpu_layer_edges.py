@@ -2,7 +2,7 @@
 their kernels take.  Tolerances are sums of roundings, as in test_gpu_layers.py."""
 import pytest
 
-from tests.test_gpu_layers import _bits, _gen, _randn, _same_selection, _select, _t, _torch
+from tests.test_gpu_layers import LEAST, U, _bits, _gen, _half_step, _randn, _same_selection, _select, _t, _torch, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +31,27 @@ def test_beam_select_signalling_nan(kind, patterns, V):
     scores = -torch.rand(n, generator=g, device="cuda")
     for allowed in (None, _bits(g, n, V, 0.7)):
         _same_selection(P.vp_beam_select(z, scores, B, allowed=allowed), _select(z, scores, B, allowed))
+
+
+# ---------------------------------------------------------------- norm
+@pytest.mark.parametrize("kind", ["bfloat16", "float32"])
+@pytest.mark.parametrize("size", [1e-16, 1e-13, 3e11, 1e14, 1e17])
+@pytest.mark.parametrize("d", [96, 1500])
+def test_add_norm_grad_of_rows_of_any_size(kind, size, d):
+    """Rows so small or so large that rstd^3 is no number of 32 bits any more, though rstd is."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    n = 37
+    g = _gen(d)
+    s, dn = _randn(g, (n, d), kind, size), _randn(g, (n, d), kind)
+    w = (1 + _randn(g, (d,), "float32", 0.1)).to(_t(kind))
+    r = torch.rsqrt(s.double().square().mean(1)).float()      # (eps = 0)
+    dx, dw = P.vp_add_norm_grad(dn, s, w, r)
+    rd = r.double()[:, None]
+    h, wdy = s.double() * rd, dn.double() * w.double()
+    want = rd * (wdy - h * (wdy * h).mean(1, keepdim=True))
+    chain = 8 + 6 + -(-d // 512)       # a lane's eight products, six joins of the lanes, the wavefronts
+    bound = U * rd * (4 * wdy.abs() + h.abs() * (wdy * h).abs().mean(1, keepdim=True) * (chain + 8))
+    _within(dx, want, bound + (want.abs() + bound) * _half_step(kind) + LEAST[kind])
+    # one product rounds h, one the term; rows of a wavefront, and its joins, one by one at most
+    _within(dw, (dn.double() * h).sum(0), (dn.double() * h).abs().sum(0) * (n + 2) * U)
