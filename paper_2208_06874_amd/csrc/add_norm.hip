@@ -176,7 +176,7 @@ __global__ __launch_bounds__(64 * waves_of(W)) void add_norm_grad_kernel(const N
         to.f.load((const T *)A.s + (size_t)at * A.s_stride, c, d);
         to.g.load((const T *)A.dnorm + (size_t)at * A.dnorm_stride, c, d);
         if (A.dsum) to.e.load((const T *)A.dsum + (size_t)at * A.dsum_stride, c, d);
-        to.r = row < A.n ? A.rstd[at] : 0.f;
+        to.r = A.rstd[at];
     };
     const long mine = (long)blockIdx.x * ROWS, step = (long)gridDim.x * ROWS;
     if (mine < A.n) load(mine + wave / W, next);
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(64 * waves_of(W)) void add_norm_grad_kernel(const N
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             f[j] *= r;
-            dw[j] += g[j] * f[j];
+            dw[j] = row < A.n ? fmaf(g[j], f[j], dw[j]) : dw[j];     // (not by r = 0: the row that is read may hold infinities)
             g[j] *= w[j];
             dot += g[j] * f[j];
         }

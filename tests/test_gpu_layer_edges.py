@@ -1,5 +1,7 @@
 """Calls of the layers next to the projection where they can go wrong: values, sizes and lists at the borders of what
 their kernels take.  Tolerances are sums of roundings, as in test_gpu_layers.py."""
+import math
+
 import pytest
 
 from tests.test_gpu_layers import LEAST, U, _bits, _gen, _half_step, _randn, _same_selection, _select, _t, _torch, _within
@@ -55,3 +57,18 @@ def test_add_norm_grad_of_rows_of_any_size(kind, size, d):
     _within(dx, want, bound + (want.abs() + bound) * _half_step(kind) + LEAST[kind])
     # one product rounds h, one the term; rows of a wavefront, and its joins, one by one at most
     _within(dw, (dn.double() * h).sum(0), (dn.double() * h).abs().sum(0) * (n + 2) * U)
+
+
+@pytest.mark.parametrize("n,d", [(1, 64), (5, 64), (7, 600), (2, 2000), (4101, 200)])
+def test_add_norm_grad_infinity_in_the_last_row(n, d):
+    """Rows are taken four or two at a time: those past the last one count nothing, whatever the last one holds."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    s, dn = torch.ones((n, d), device="cuda"), torch.ones((n, d), device="cuda")
+    dn[n - 1, 3] = math.inf
+    dn[n - 1, d - 1] = -math.inf
+    dx, dw = P.vp_add_norm_grad(dn, s, torch.ones(d, device="cuda"), torch.ones(n, device="cuda"))
+    want = torch.full((d,), float(n), device="cuda")
+    want[3], want[d - 1] = math.inf, -math.inf
+    assert torch.equal(dw, want)
+    assert torch.isfinite(dx[:n - 1]).all() and dx[n - 1].isnan().all()      # (inf - inf is in the last row's mean)
