@@ -72,3 +72,21 @@ def test_add_norm_grad_infinity_in_the_last_row(n, d):
     want[3], want[d - 1] = math.inf, -math.inf
     assert torch.equal(dw, want)
     assert torch.isfinite(dx[:n - 1]).all() and dx[n - 1].isnan().all()      # (inf - inf is in the last row's mean)
+
+
+@pytest.mark.parametrize("d", [1, 65, 300, 513, 2500, 4095])
+def test_add_norm_pads_with_zeros_whatever_the_row_holds(d):
+    """Columns past d of a row with NaN or infinities, and of one so small that rstd is infinite (eps = 0), are zeros and
+    take no part in the last block's scale."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    x = torch.ones((4, d), device="cuda")
+    x[1, d // 2] = math.nan
+    x[2, d // 2] = math.inf
+    x[3] = 1e-30                            # (its square is no number above zero: rstd is infinite, and so is y)
+    got = P.vp_add_norm(x, torch.ones(d, device="cuda"), eps=0.0, quantize=True, norm_dtype=torch.float32)
+    width = -(-d // 128) * 128
+    rows = got.q.as_strided((4, width), (width, 1)).view(torch.uint8)
+    assert not rows[:, d:].any()
+    assert got.norm[3].isinf().all() and got.scales[3].isinf().all() and got.scales[1].isnan().all()
+    assert torch.equal(got.scales[0], torch.full_like(got.scales[0], 1.0 / 448))
