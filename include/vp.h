@@ -430,6 +430,10 @@ typedef struct {
 vp_status vp_beam_reorder(const vp_state *states, int32_t count, const int32_t *parent, int32_t S, int32_t B,
                           void *hip_stream);
 
+/* Whether vp_beam_reorder takes these states, without moving them: for callers whose states need several calls, none of
+ * which may move anything before all of them are known to be taken. */
+vp_status vp_beam_reorder_check(const vp_state *states, int32_t count, int32_t S, int32_t B);
+
 /* Host utility: v rounded to fp16 bits exactly as vp_kmeans rounds a mean. */
 uint16_t vp_round_to_half(double v);
 

@@ -763,6 +763,68 @@ vp_status select_sizes(const char *fn, int32_t S, int32_t B, int32_t V)
     return VP_OK;
 }
 
+// What a reorder needs to know of its states, or why there is none: nothing is launched.
+vp_status reorder_states(const vp_state *states, int32_t count, int32_t S, int32_t B, ReorderArgs *A, long *groups_in_all)
+{
+    if (S < 0 || B < 1 || B > VP_MAX_BEAMS || (long)S * B > VP_MAX_ROWS)
+        return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_reorder: S = %d, B = %d (need 1 <= B <= %d, S * B <= %d)", S, B, VP_MAX_BEAMS, VP_MAX_ROWS);
+    if (count < 0 || count > STATES) return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_reorder: %d states: at most %d a call", count, STATES);
+    if (count > 0 && !states) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: null pointer argument");
+    long total = 0;
+    for (int i = 0; i < count; ++i) {
+        const vp_state &in = states[i];
+        if (in.elem_bytes != 1 && in.elem_bytes != 2 && in.elem_bytes != 4 && in.elem_bytes != 8)
+            return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d: elements of %d bytes", i, in.elem_bytes);
+        if (in.dims < 1 || in.dims > VP_STATE_DIMS || in.row_dim < 0 || in.row_dim >= in.dims)
+            return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d: %d dimensions, rows along %d", i, in.dims, in.row_dim);
+        if (in.sizes[in.row_dim] != (int64_t)S * B)
+            return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d has %lld rows, %lld hypotheses", i, (long long)in.sizes[in.row_dim], (long long)S * B);
+        // the dimensions by stride; they must not overlap (what lies inside a step is smaller than the step)
+        int order[VP_STATE_DIMS], kept = 0;
+        bool empty = S == 0;
+        for (int j = 0; j < in.dims; ++j) {
+            if (in.sizes[j] < 0 || in.strides[j] < 0) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d: a negative size or stride", i);
+            empty = empty || in.sizes[j] == 0;
+            if (in.sizes[j] > 1) order[kept++] = j;
+        }
+        if (empty) continue;
+        if (!in.data || !layer_aligned(in.data, in.elem_bytes)) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d: null or misaligned address", i);
+        std::sort(order, order + kept, [&](int a, int b) { return in.strides[a] < in.strides[b]; });
+        int64_t reach = 1;
+        for (int j = 0; j < kept; ++j) {
+            if (in.strides[order[j]] < reach) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d overlaps itself", i);
+            reach = (in.sizes[order[j]] - 1) * in.strides[order[j]] + reach;
+        }
+        StateArgs &st = A->state[A->states];
+        st.base = (char *)in.data;
+        st.elem = in.elem_bytes;
+        st.row_stride = (long)in.strides[in.row_dim] * in.elem_bytes;
+        st.run = in.elem_bytes;
+        // dimensions that continue each other become one; those that continue the run lengthen it
+        for (int j = 0; j < kept; ++j) {
+            const int o = order[j];
+            if (o == in.row_dim) continue;
+            const long size = (long)in.sizes[o], stride = (long)in.strides[o] * in.elem_bytes;
+            if (st.dims == 0 && stride == st.run) st.run *= size;
+            else if (st.dims > 0 && stride == st.sizes[st.dims - 1] * st.strides[st.dims - 1]) st.sizes[st.dims - 1] *= size;
+            else if (st.dims == DIMS) return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_reorder: state %d: more than %d separate dimensions around its runs", i, DIMS);
+            else st.sizes[st.dims] = size, st.strides[st.dims++] = stride;
+        }
+        const long chunks = st.run / 16 + st.run % 16 / st.elem;
+        long places = 1;
+        for (int j = 0; j < st.dims; ++j) places *= st.sizes[j];
+        const long groups = layer_ceil_div(chunks * places, THREADS);
+        if (chunks * places >= (1l << 31) || total + groups * S >= (1l << 31))   // (places are numbered in 32 bits)
+            return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_reorder: state %d is too large", i);
+        st.chunks = (unsigned int)chunks;
+        st.groups = (unsigned int)groups;
+        total += groups * S;
+        ++A->states;
+    }
+    *groups_in_all = total;
+    return VP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -820,68 +882,24 @@ vp_status vp_beam_select(const void *logits, int32_t type, int64_t stride, const
     return VP_OK;
 }
 
+vp_status vp_beam_reorder_check(const vp_state *states, int32_t count, int32_t S, int32_t B)
+{
+    ReorderArgs A = {};
+    long total = 0;
+    return reorder_states(states, count, S, B, &A, &total);
+}
+
 vp_status vp_beam_reorder(const vp_state *states, int32_t count, const int32_t *parent, int32_t S, int32_t B,
                           void *hip_stream)
 {
-    if (S < 0 || B < 1 || B > VP_MAX_BEAMS || (long)S * B > VP_MAX_ROWS)
-        return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_reorder: S = %d, B = %d (need 1 <= B <= %d, S * B <= %d)", S, B, VP_MAX_BEAMS, VP_MAX_ROWS);
-    if (count < 0 || count > STATES) return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_reorder: %d states: at most %d a call", count, STATES);
-    if ((count > 0 && !states) || (S > 0 && count > 0 && !parent)) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: null pointer argument");
     ReorderArgs A = {};
+    long total = 0;
+    const vp_status s = reorder_states(states, count, S, B, &A, &total);
+    if (s != VP_OK) return s;
+    if (S > 0 && count > 0 && !parent) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: null pointer argument");
     A.S = S;
     A.B = B;
     A.parent = parent;
-    long total = 0;
-    for (int i = 0; i < count; ++i) {
-        const vp_state &in = states[i];
-        if (in.elem_bytes != 1 && in.elem_bytes != 2 && in.elem_bytes != 4 && in.elem_bytes != 8)
-            return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d: elements of %d bytes", i, in.elem_bytes);
-        if (in.dims < 1 || in.dims > VP_STATE_DIMS || in.row_dim < 0 || in.row_dim >= in.dims)
-            return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d: %d dimensions, rows along %d", i, in.dims, in.row_dim);
-        if (in.sizes[in.row_dim] != (int64_t)S * B)
-            return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d has %lld rows, %lld hypotheses", i, (long long)in.sizes[in.row_dim], (long long)S * B);
-        // the dimensions by stride; they must not overlap (what lies inside a step is smaller than the step)
-        int order[VP_STATE_DIMS], kept = 0;
-        bool empty = S == 0;
-        for (int j = 0; j < in.dims; ++j) {
-            if (in.sizes[j] < 0 || in.strides[j] < 0) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d: a negative size or stride", i);
-            empty = empty || in.sizes[j] == 0;
-            if (in.sizes[j] > 1) order[kept++] = j;
-        }
-        if (empty) continue;
-        if (!in.data || !layer_aligned(in.data, in.elem_bytes)) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d: null or misaligned address", i);
-        std::sort(order, order + kept, [&](int a, int b) { return in.strides[a] < in.strides[b]; });
-        int64_t reach = 1;
-        for (int j = 0; j < kept; ++j) {
-            if (in.strides[order[j]] < reach) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d overlaps itself", i);
-            reach = (in.sizes[order[j]] - 1) * in.strides[order[j]] + reach;
-        }
-        StateArgs &st = A.state[A.states];
-        st.base = (char *)in.data;
-        st.elem = in.elem_bytes;
-        st.row_stride = (long)in.strides[in.row_dim] * in.elem_bytes;
-        st.run = in.elem_bytes;
-        // dimensions that continue each other become one; those that continue the run lengthen it
-        for (int j = 0; j < kept; ++j) {
-            const int o = order[j];
-            if (o == in.row_dim) continue;
-            const long size = (long)in.sizes[o], stride = (long)in.strides[o] * in.elem_bytes;
-            if (st.dims == 0 && stride == st.run) st.run *= size;
-            else if (st.dims > 0 && stride == st.sizes[st.dims - 1] * st.strides[st.dims - 1]) st.sizes[st.dims - 1] *= size;
-            else if (st.dims == DIMS) return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_reorder: state %d: more than %d separate dimensions around its runs", i, DIMS);
-            else st.sizes[st.dims] = size, st.strides[st.dims++] = stride;
-        }
-        const long chunks = st.run / 16 + st.run % 16 / st.elem;
-        long places = 1;
-        for (int j = 0; j < st.dims; ++j) places *= st.sizes[j];
-        const long groups = layer_ceil_div(chunks * places, THREADS);
-        if (chunks * places >= (1l << 31) || total + groups * S >= (1l << 31))   // (places are numbered in 32 bits)
-            return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_reorder: state %d is too large", i);
-        st.chunks = (unsigned int)chunks;
-        st.groups = (unsigned int)groups;
-        total += groups * S;
-        ++A.states;
-    }
     if (total == 0 || B == 1) return VP_OK;
     const hipStream_t st = (hipStream_t)hip_stream;
     const dim3 grid((unsigned int)total);

@@ -296,7 +296,7 @@ class State(ctypes.Structure):
 def vp_beam_reorder(states: Sequence[Tuple], parent, B: int, stream=None):
     """Moves what belongs to the hypotheses, in place: along dimension `dim` of every (tensor, dim), row s * B + b
     becomes what row s * B + parent[s * B + b] was; rows with a parent outside [0, B) stay.  Tensors may be views
-    with any strides that do not overlap themselves (nor each other)."""
+    with any strides that do not overlap themselves (nor each other).  Where one of them is refused, none has moved."""
     torch = _torch()
     _want(parent, "parent", torch.int32)
     _same_device(parent, "parent")
@@ -318,6 +318,10 @@ def vp_beam_reorder(states: Sequence[Tuple], parent, B: int, stream=None):
         k = t.dim()
         described.append(State(t.data_ptr(), t.element_size(), k, dim % k, (ctypes.c_int64 * STATE_DIMS)(*t.shape),
                                (ctypes.c_int64 * STATE_DIMS)(*t.stride())))
-    for at in range(0, len(described), MAX_STATES):
-        part = described[at:at + MAX_STATES]
-        _check(lib().vp_beam_reorder((State * len(part))(*part), len(part), parent.data_ptr(), n // B, B, _handle(stream, parent.device)))
+    parts = [described[at:at + MAX_STATES] for at in range(0, len(described), MAX_STATES)]
+    parts = [((State * len(part))(*part), len(part)) for part in parts]
+    if len(parts) > 1:      # (nothing moves before all of them are known to be taken)
+        for part, k in parts:
+            _check(lib().vp_beam_reorder_check(part, k, n // B, B))
+    for part, k in parts:
+        _check(lib().vp_beam_reorder(part, k, parent.data_ptr(), n // B, B, _handle(stream, parent.device)))

@@ -26,7 +26,7 @@ EXPORTS = ("vp_build_bytes", "vp_build", "vp_get_info", "vp_set_option", "vp_wor
            "vp_round_to_half", "vp_beam_step", "vp_measure_ceilings",
            "vp_embed", "vp_embed_grad_workspace_bytes", "vp_embed_grad", "vp_add_norm", "vp_add_norm_grad_workspace_bytes",
            "vp_add_norm_grad", "vp_scaled_pack_bytes", "vp_scaled_pack", "vp_scaled_matmul_workspace_bytes",
-           "vp_scaled_matmul", "vp_beam_select_workspace_bytes", "vp_beam_select", "vp_beam_reorder")
+           "vp_scaled_matmul", "vp_beam_select_workspace_bytes", "vp_beam_select", "vp_beam_reorder", "vp_beam_reorder_check")
 
 
 class VpError(RuntimeError):
@@ -119,7 +119,8 @@ def lib():
                 ("vp_scaled_matmul", i32, (vp, i32, i32, vp, i64, vp, i32, vp, i32, vp, i32, vp, size, vp)),
                 ("vp_beam_select_workspace_bytes", size, (i32, i32, i32)),
                 ("vp_beam_select", i32, (vp, i32, i64, vp, i32, i32, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp, size, vp)),
-                ("vp_beam_reorder", i32, (vp, i32, vp, i32, i32, vp))):
+                ("vp_beam_reorder", i32, (vp, i32, vp, i32, i32, vp)),
+                ("vp_beam_reorder_check", i32, (vp, i32, i32, i32))):
             getattr(L, name).restype, getattr(L, name).argtypes = result, args
         L.vp_round_to_half.restype = ctypes.c_uint16
         L.vp_round_to_half.argtypes = [ctypes.c_double]

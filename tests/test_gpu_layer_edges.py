@@ -90,3 +90,22 @@ def test_add_norm_pads_with_zeros_whatever_the_row_holds(d):
     assert not rows[:, d:].any()
     assert got.norm[3].isinf().all() and got.scales[3].isinf().all() and got.scales[1].isnan().all()
     assert torch.equal(got.scales[0], torch.full_like(got.scales[0], 1.0 / 448))
+
+
+# ---------------------------------------------------------------- reordering
+@pytest.mark.parametrize("bad", [8, 12, 17])
+def test_beam_reorder_moves_all_or_nothing(bad):
+    """More states than one call of the library takes, one of them refused: the others stay as they are."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    parent = torch.tensor([1, 1, 0, 2, 0, 0], dtype=torch.int32, device="cuda")
+    states = [(torch.arange(6.0, device="cuda")[:, None] + torch.arange(5.0, device="cuda") * 10 + i, 0) for i in range(18)]
+    kept = [t.clone() for t, _ in states]
+    wrong = list(states)
+    wrong[bad] = (torch.zeros((6, 1), device="cuda").expand(6, 4), 0)
+    with pytest.raises(P.VpError, match="overlaps"):
+        P.vp_beam_reorder(wrong, parent, 3)
+    assert all(torch.equal(t, k) for (t, _), k in zip(states, kept))
+    P.vp_beam_reorder(states, parent, 3)
+    at = torch.tensor([1, 1, 0, 5, 3, 3], device="cuda")
+    assert all(torch.equal(t, k[at]) for (t, _), k in zip(states, kept))

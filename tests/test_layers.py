@@ -121,3 +121,16 @@ def test_binding_refuses_host_tensors_and_wrong_types_before_any_c_call():
         P.vp_scaled_pack(h, torch.ones(1, 1))
     with pytest.raises(ValueError, match="one of"):
         layers._type_code(torch.float64, "t")
+
+
+@pytest.mark.parametrize("state,kw,status", [
+    (_state([6, 8], [8, 1]), {}, OK), (_state([6, 8], [8, 0]), {}, INVALID), (_state([5, 8], [8, 1]), {}, INVALID), (_state([6, 8], [8, 1], elem=3), {}, INVALID),
+    (_state([6, 2, 2, 2, 2, 2], [1000, 2, 8, 32, 128, 512]), {}, UNSUPPORTED), (_state([6, 8], [8, 1]), dict(count=9), UNSUPPORTED),
+    (_state([6, 8], [8, 1]), dict(B=33, S=1), UNSUPPORTED), (_state([6, 8], [8, 1], data=None), dict(count=0), OK)])
+def test_reorder_check_says_what_reorder_would(state, kw, status):
+    a = dict(dict(count=1, S=2, B=3), **kw)
+    assert vp.lib().vp_beam_reorder_check(ctypes.byref(state), a["count"], a["S"], a["B"]) == status, vp.last_error()
+    if status != OK:
+        said = vp.last_error()
+        assert vp.lib().vp_beam_reorder(ctypes.byref(state), a["count"], A, a["S"], a["B"], None) == status and vp.last_error() == said
+    assert vp.lib().vp_beam_reorder_check(None, 1, 2, 3) == INVALID
