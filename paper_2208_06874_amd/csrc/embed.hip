@@ -578,12 +578,16 @@ vp_status vp_embed(const void *table, int32_t table_type, int64_t table_stride, 
         return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_embed: an address that is no multiple of its element's size");
     int row_threads = 4;
     while (row_threads < THREADS && row_threads * (int)(16 / type_size(out_type)) < d) row_threads *= 2;
-    const dim3 grid((unsigned int)layer_ceil_div(n, THREADS / row_threads));
+    const long most = LAUNCH_THREADS / row_threads;
+    const bool stream = n * d * (long)type_size(out_type) > STREAM_BYTES;
     with_type(table_type, [&](auto t) {
         with_type(out_type, [&](auto o) {
-            hipLaunchKernelGGL((embed_kernel<decltype(t), decltype(o)>), grid, dim3(THREADS), 0, (hipStream_t)hip_stream,
-                               (const decltype(t) *)table, (long)table_stride, V, d, ids, (long)n, scale, row_threads, n * d * (long)type_size(out_type) > STREAM_BYTES,
-                               (decltype(o) *)out);
+            for (long at = 0; at < n; at += most) {
+                const long rows = std::min<long>(most, n - at);
+                hipLaunchKernelGGL((embed_kernel<decltype(t), decltype(o)>), dim3((unsigned int)layer_ceil_div(rows, THREADS / row_threads)), dim3(THREADS), 0,
+                                   (hipStream_t)hip_stream, (const decltype(t) *)table, (long)table_stride, V, d, ids + at, rows, scale, row_threads, stream,
+                                   (decltype(o) *)out + at * d);
+            }
         });
     });
     const hipError_t e = hipGetLastError();

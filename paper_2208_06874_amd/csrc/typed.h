@@ -263,6 +263,10 @@ template <typename F> inline void with_type(int t, F f)
     else f(float{});
 }
 
+// A launch counts the threads of a dimension in 32 bits: calls of more rows than fit take several launches of at most these
+// many threads.
+constexpr long LAUNCH_THREADS = 1l << 31;
+
 constexpr size_t LAYER_ALIGN = 256;
 inline size_t layer_align_up(size_t x) { return (x + LAYER_ALIGN - 1) / LAYER_ALIGN * LAYER_ALIGN; }
 inline bool layer_aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }

@@ -109,3 +109,32 @@ def test_beam_reorder_moves_all_or_nothing(bad):
     P.vp_beam_reorder(states, parent, 3)
     at = torch.tensor([1, 1, 0, 5, 3, 3], device="cuda")
     assert all(torch.equal(t, k[at]) for (t, _), k in zip(states, kept))
+
+
+# ---------------------------------------------------------------- more rows than the threads of one launch
+def _room(gigabytes):
+    """Skips where the card has not this much memory free."""
+    torch = _torch()
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gigabytes * 1.2e9:
+        pytest.skip("needs %d GB of GPU memory" % gigabytes)
+
+
+@pytest.mark.parametrize("n,d", [(2 ** 30 + 77, 1), (2 ** 24 + 3, 520)])
+def test_embed_of_more_rows_than_a_launch_has_threads(n, d):
+    """Four threads a row at least and 256 at most: 2^32 threads and more, and what lies on both sides of where launches meet."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    _room(50)
+    V = 1000
+    t = _randn(_gen(d), (V, d), "float32")
+    ids = torch.arange(n, device="cuda", dtype=torch.int32) % V
+    ids[5::1 << 20] = -1
+    got = P.vp_embed(t, ids)
+    at = torch.cat([torch.arange(s, min(s + 2000, n), device="cuda") for s in (0, 2 ** 23 - 1000, 2 ** 24 - 1000, 2 ** 29 - 1000, 2 ** 30 - 1000, n - 2000) if s < n])
+    want = torch.where(ids[at, None] >= 0, t[ids[at].long().clamp(min=0)], 0.0)
+    assert torch.equal(got[at], want)
+    step = max(1, 2 ** 26 // d)
+    for a in range(0, n, step):              # every row was written
+        i = ids[a:a + step].long()
+        assert torch.equal(got[a:a + step, 0], torch.where(i >= 0, t[i.clamp(min=0), 0], 0.0)), a
