@@ -61,6 +61,18 @@ struct NormArgs {
     float *scales;
     float *rstd;
     bool stream;
+
+    // on to the rows behind these (elements of `size` bytes)
+    void skip(long rows, size_t size)
+    {
+        const long blocks = (d + BLOCK - 1) / BLOCK;
+        x = (const char *)x + rows * x_stride * size;
+        if (residual) residual = (const char *)residual + rows * residual_stride * size;
+        if (sum) sum = (char *)sum + rows * d * size;
+        if (norm) norm = (char *)norm + rows * d * type_size(norm_type);
+        if (q) q += rows * blocks * BLOCK, scales += rows * blocks;
+        if (rstd) rstd += rows;
+    }
 };
 
 // Sum over the W wavefronts of a row; `slot`: one of two places, in turn where calls follow each other.
@@ -291,12 +303,17 @@ vp_status vp_add_norm(const void *x, int64_t x_stride, const void *residual, int
     if (!layer_aligned(x, a) || !layer_aligned(residual, a) || !layer_aligned(sum, a) || !layer_aligned(weight, type_size(weight_type)) ||
         (norm && !layer_aligned(norm, type_size(norm_type))) || !layer_aligned(q, 8) || !layer_aligned(scales, 4) || !layer_aligned(rstd, 4))
         return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_add_norm: an address that is no multiple of its element's size (q: of 8)");
-    const NormArgs A = {x, residual, weight, (long)x_stride, (long)residual_stride, (long)n, d, weight_type, eps, sum, norm, norm_type, q, scales, rstd,
-                        n * d * (long)((sum ? a : 0) + (norm ? type_size(norm_type) : 0) + (q ? 1 : 0)) > STREAM_BYTES};
-    const dim3 grid((unsigned int)layer_ceil_div(n, rows_at_once(d)));
+    NormArgs A = {x, residual, weight, (long)x_stride, (long)residual_stride, 0, d, weight_type, eps, sum, norm, norm_type, q, scales, rstd,
+                  n * d * (long)((sum ? a : 0) + (norm ? type_size(norm_type) : 0) + (q ? 1 : 0)) > STREAM_BYTES};
     with_type(type, [&](auto t) {
         with_waves(d, [&](auto waves) {
-            hipLaunchKernelGGL((add_norm_kernel<decltype(t), decltype(waves)::value>), grid, dim3(64 * waves_of(decltype(waves)::value)), 0, (hipStream_t)hip_stream, A);
+            constexpr int W = decltype(waves)::value, ROWS = waves_of(W) / W;
+            constexpr long most = LAUNCH_THREADS / (64 * W);
+            for (long at = 0; at < n; at += most) {
+                A.n = std::min<long>(most, n - at);
+                hipLaunchKernelGGL((add_norm_kernel<decltype(t), W>), dim3((unsigned int)layer_ceil_div(A.n, ROWS)), dim3(64 * waves_of(W)), 0, (hipStream_t)hip_stream, A);
+                A.skip(most, a);
+            }
         });
     });
     const hipError_t e = hipGetLastError();

@@ -138,3 +138,27 @@ def test_embed_of_more_rows_than_a_launch_has_threads(n, d):
     for a in range(0, n, step):              # every row was written
         i = ids[a:a + step].long()
         assert torch.equal(got[a:a + step, 0], torch.where(i >= 0, t[i.clamp(min=0), 0], 0.0)), a
+
+
+@pytest.mark.parametrize("n,d", [(2 ** 26 + 5, 8), (2 ** 25 + 3, 520)])
+def test_add_norm_of_more_rows_than_a_launch_has_threads(n, d):
+    """64 threads a row, and 128.  The rows are a few, over and over: equal rows give equal results."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    _room(20 + 7 * n * d / 1e9)      # (four of 16 bits, rows of q at multiples of 128 bytes)
+    few = 61
+    g = _gen(d)
+    rows, rest, w = _randn(g, (few, d), "bfloat16"), _randn(g, (few, d), "bfloat16"), _randn(g, (d,), "float32")
+    x, r = rows.repeat(-(-n // few), 1)[:n], rest.repeat(-(-n // few), 1)[:n]
+    want = P.vp_add_norm(rows, w, residual=rest, norm_dtype=torch.bfloat16, quantize=True, rstd=True)
+    got = P.vp_add_norm(x, w, residual=r, norm_dtype=torch.bfloat16, quantize=True, rstd=True, inplace=True)
+    assert got.sum is r
+    step = few * (2 ** 24 // d + 1)
+    for a in range(0, n, step):
+        for name in ("sum", "norm", "q", "scales", "rstd"):
+            here, base = getattr(got, name)[a:a + step], getattr(want, name)
+            if name == "q":
+                here, base = here.view(torch.uint8), base.view(torch.uint8)
+            whole = here.shape[0] // few * few
+            assert (here[:whole].view(-1, *base.shape) == base).all() if here.is_contiguous() else (here[:whole].unflatten(0, (-1, few)) == base).all(), (name, a)
+            assert torch.equal(here[whole:], base[:here.shape[0] - whole]), (name, a)
