@@ -339,7 +339,7 @@ typedef enum { VP_F16 = 0, VP_BF16 = 1, VP_F32 = 2 } vp_type;
 /* out[i, :] = scale * table[ids[i], :], computed in 32 bits and rounded once; ids outside [0, V) (such as the -1 of a
  * missing hypothesis) give rows of zeros.
  *   table  device, table_type [V, d];  ids  device, int32 [n];  out  device, out_type [n, d]
- * Limits: 1 <= d <= 4096, 0 <= n < 2^31 - 65536. */
+ * Limits: 1 <= d <= 4096, 1 <= V < 2^31 - 16, 0 <= n < 2^31 - 65536. */
 vp_status vp_embed(const void *table, int32_t table_type, int64_t table_stride, int32_t V, int32_t d,
                    const int32_t *ids, int64_t n, float scale, void *out, int32_t out_type, void *hip_stream);
 

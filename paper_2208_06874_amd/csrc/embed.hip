@@ -318,14 +318,14 @@ __device__ void grad_item(const T *__restrict__ dout, long stride, long n, int d
 }
 
 // Workgroups 0 .. item_groups - 1 take the windows of long lists, so that these begin first; the others write the
-// rows of TOKENS tokens each, a wavefront a row: zeros, or the sum over its list, ordered by counting.
+// rows of TOKENS tokens each from `first` on, a wavefront a row: zeros, or the sum over its list, ordered by counting.
 template <typename T, typename G>
 __global__ __launch_bounds__(THREADS) void grad_rows_kernel(const T *__restrict__ dout, long stride, long n, int V,
                                                             int d, float scale, const int32_t *__restrict__ count,
                                                             const int32_t *__restrict__ start,
                                                             const int32_t *__restrict__ list,
                                                             const GradState *__restrict__ state,
-                                                            const GradItem *__restrict__ items, int item_groups,
+                                                            const GradItem *__restrict__ items, int item_groups, long first,
                                                             float *__restrict__ partial, G *__restrict__ grad)
 {
     __shared__ ItemRoom R;
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(THREADS) void grad_rows_kernel(const T *__restrict_
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // a wavefront's four tokens; their lists, 16 lanes each, in one load, and ordered by counting: a lane's place is the
     // number of smaller positions among its 16
-    const long t0 = (long)(blockIdx.x - item_groups) * TOKENS + wave * (TOKENS / 4);
+    const long t0 = first + (long)(blockIdx.x - item_groups) * TOKENS + wave * (TOKENS / 4);
     const long mine = t0 + (lane >> 4);
     const int many = mine < V ? count[mine] : -1;
     const int at = lane & 15;
@@ -431,7 +431,7 @@ constexpr int FEW = 1024, TOGETHER = 32;
 template <int TAKEN, typename T, typename G>
 __global__ __launch_bounds__(THREADS) void grad_few_kernel(const T *__restrict__ dout, long stride,
                                                            const int32_t *__restrict__ ids, int n, int V, int d,
-                                                           float scale, int padding_id, G *__restrict__ grad)
+                                                           float scale, int padding_id, int first, G *__restrict__ grad)
 {
     constexpr int E = LANE_ELEMENTS<G>, PER = FEW / THREADS;
     __shared__ uint32_t list[FEW];               // (token - t0) * 2^16 + position, ascending positions
@@ -439,14 +439,14 @@ __global__ __launch_bounds__(THREADS) void grad_few_kernel(const T *__restrict__
     __shared__ int many[TAKEN], sums[WAVES];
     __shared__ float part[WAVES - 1][64 * E];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int t0 = blockIdx.x * TAKEN, c = blockIdx.y * 64 * E + lane * E;
+    const int t0 = first + (int)blockIdx.x * TAKEN, c = blockIdx.y * 64 * E + lane * E;
     if (threadIdx.x < TAKEN) many[threadIdx.x] = 0;
     int id[PER], found = 0;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
         const int i = threadIdx.x * PER + u;
         id[u] = i < n ? ids[i] : -1;
-        if (!counts(id[u], V, padding_id) || id[u] < t0 || id[u] >= t0 + TAKEN) id[u] = -1;
+        if (!counts(id[u], V, padding_id) || id[u] < t0 || id[u] - t0 >= TAKEN) id[u] = -1;
         found += id[u] >= 0;
     }
     const int upto = wave_inclusive_sum(found);
@@ -486,7 +486,7 @@ __global__ __launch_bounds__(THREADS) void grad_few_kernel(const T *__restrict__
     // tokens by 64: every fourth is this wavefront's, those of long lists all wavefronts'
     constexpr unsigned long long FOURTH = 0x1111111111111111ull;
     for (int h = 0; h < TAKEN; h += 64) {
-        const int of = h + lane < TAKEN && t0 + h + lane < V ? many[(h + lane) & (TAKEN - 1)] : -1;
+        const int of = h + lane < min(TAKEN, V - t0) ? many[(h + lane) & (TAKEN - 1)] : -1;
         unsigned long long some = __ballot(of > 0 && of <= TOGETHER) & FOURTH << wave, none = narrow ? 0 : __ballot(of == 0) & FOURTH << wave;
         for (; none; none &= none - 1) {
             const float zero[E] = {};
@@ -622,13 +622,16 @@ vp_status vp_embed_grad(const void *dout, int32_t dout_type, int64_t dout_stride
     if (n <= FEW) {
         auto launch = [&](auto taken) {
             constexpr int TAKEN = decltype(taken)::value;
-            const dim3 grid((unsigned int)layer_ceil_div(V, TAKEN), (unsigned int)layer_ceil_div(d, 64 * (16 / type_size(grad_type))));
-            with_type(dout_type, [&](auto t) {
-                with_type(grad_type, [&](auto g) {
-                    hipLaunchKernelGGL((grad_few_kernel<TAKEN, decltype(t), decltype(g)>), grid, dim3(THREADS), 0, st, (const decltype(t) *)dout,
-                                       (long)dout_stride, ids, (int)n, V, d, scale, padding_id, (decltype(g) *)grad);
+            constexpr long most = LAUNCH_THREADS / THREADS;      // workgroups of a launch
+            for (long at = 0; at < layer_ceil_div(V, TAKEN); at += most) {
+                const dim3 grid((unsigned int)std::min<long>(most, layer_ceil_div(V, TAKEN) - at), (unsigned int)layer_ceil_div(d, 64 * (16 / type_size(grad_type))));
+                with_type(dout_type, [&](auto t) {
+                    with_type(grad_type, [&](auto g) {
+                        hipLaunchKernelGGL((grad_few_kernel<TAKEN, decltype(t), decltype(g)>), grid, dim3(THREADS), 0, st, (const decltype(t) *)dout,
+                                           (long)dout_stride, ids, (int)n, V, d, scale, padding_id, (int)(at * TAKEN), (decltype(g) *)grad);
+                    });
                 });
-            });
+            }
         };
         // (every workgroup looks through all ids: 500 positions in 250,000 tokens of 24 take 24 us with 32 tokens to a workgroup)
         if (V <= 32768) launch(std::integral_constant<int, 32>{});
@@ -653,14 +656,18 @@ vp_status vp_embed_grad(const void *dout, int32_t dout_type, int64_t dout_stride
     }
     const int cols = (d + ITEM_COLS - 1) / ITEM_COLS;
     const int item_groups = (int)std::min<long>(MAX_ITEM_GROUPS, L.max_items * cols);
-    const dim3 grid((unsigned int)(item_groups + layer_ceil_div(V, TOKENS)));
-    with_type(dout_type, [&](auto t) {
-        with_type(grad_type, [&](auto g) {
-            hipLaunchKernelGGL((grad_rows_kernel<decltype(t), decltype(g)>), grid, dim3(THREADS), 0, st,
-                               (const decltype(t) *)dout, (long)dout_stride, (long)n, V, d, scale, count, start, list,
-                               state, items, item_groups, partial, (decltype(g) *)grad);
+    constexpr long most = LAUNCH_THREADS / THREADS;
+    for (long at = 0; at < layer_ceil_div(V, TOKENS); at += most) {
+        const int windows = at == 0 ? item_groups : 0;
+        const dim3 grid((unsigned int)(windows + std::min<long>(most, layer_ceil_div(V, TOKENS) - at)));
+        with_type(dout_type, [&](auto t) {
+            with_type(grad_type, [&](auto g) {
+                hipLaunchKernelGGL((grad_rows_kernel<decltype(t), decltype(g)>), grid, dim3(THREADS), 0, st,
+                                   (const decltype(t) *)dout, (long)dout_stride, (long)n, V, d, scale, count, start, list,
+                                   state, items, windows, at * TOKENS, partial, (decltype(g) *)grad);
+            });
         });
-    });
+    }
     if (L.max_joins > 0)
         with_type(grad_type, [&](auto g) {
             hipLaunchKernelGGL((grad_join_kernel<decltype(g)>), dim3((unsigned int)std::min<long>(256, L.max_joins), (unsigned int)layer_ceil_div(d, THREADS)),

@@ -162,3 +162,25 @@ def test_add_norm_of_more_rows_than_a_launch_has_threads(n, d):
             whole = here.shape[0] // few * few
             assert (here[:whole].view(-1, *base.shape) == base).all() if here.is_contiguous() else (here[:whole].unflatten(0, (-1, few)) == base).all(), (name, a)
             assert torch.equal(here[whole:], base[:here.shape[0] - whole]), (name, a)
+
+
+@pytest.mark.parametrize("n,V", [(3000, 2 ** 28 + 21), (700, 2 ** 31 - 17)])
+def test_embed_grad_of_more_tokens_than_a_launch_has_threads(n, V):
+    """Through lists (16 threads a token) and without (two); tokens on both sides of where launches meet, and the last ones."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    _room(30)
+    g = _gen(n)
+    edges = [t for t in (0, 2 ** 27, 2 ** 28, 2 ** 30) if t < V] + [V]
+    near = torch.cat([torch.arange(max(0, t - 20), min(t + 20, V), device="cuda") for t in edges])
+    ids = near[torch.randint(0, len(near), (n,), generator=g, device="cuda")].to(torch.int32)
+    ids[::7] = int(near[30])                              # (a list that is cut into windows)
+    x = torch.randint(-8, 9, (n, 1), generator=g, device="cuda").half()      # (sums of whole numbers are exact)
+    grad = torch.full((V, 1), math.nan, dtype=torch.float16, device="cuda")
+    P.vp_embed_grad(x, ids, V, out=grad)
+    at, slot = torch.unique(ids.long(), return_inverse=True)
+    want = torch.zeros((len(at), 1), device="cuda").index_add_(0, slot, x.float())
+    assert torch.equal(grad[at].float(), want)
+    grad[at] = 0
+    for a in range(0, V, 2 ** 28):
+        assert not grad[a:a + 2 ** 28].view(torch.int16).any(), a
