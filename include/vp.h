@@ -420,6 +420,8 @@ vp_status vp_beam_select(const void *logits, int32_t type, int64_t stride, const
  * s * B + parent[s * B + b] was.  Rows whose parent is outside [0, B) (vp_beam_step's -1) stay as they are.
  *   states  host, at most 8: any strided arrays that do not overlap themselves or each other; rows along row_dim
  *           (of size S * B), sizes and strides in elements, innermost anywhere
+ *           A state is at most 2^31 - 1 pieces of 16 bytes (or of one element, where its rows' elements are apart or at the
+ *           end of a run) for each row, in at most four dimensions that do not continue each other
  *   parent  device, int32 [S * B] */
 typedef struct {
     void *data;          /* device */

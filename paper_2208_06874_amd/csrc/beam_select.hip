@@ -671,6 +671,7 @@ struct ReorderArgs {
     StateArgs state[STATES];
     int states, S, B;
     const int32_t *parent;
+    long first;            // the launch's first workgroup, of those that all states need
 };
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -699,7 +700,7 @@ __device__ inline void store_chunk(char *p, bool whole, int elem, i32x4 v)
 template <int MOST>
 __global__ __launch_bounds__(THREADS) void reorder_kernel(const ReorderArgs A)
 {
-    long group = blockIdx.x;
+    long group = A.first + blockIdx.x;
     int k = 0;
     while (k + 1 < A.states && group >= (long)A.state[k].groups * A.S) group -= (long)A.state[k].groups * A.S, ++k;
     const StateArgs &st = A.state[k];
@@ -814,7 +815,7 @@ vp_status reorder_states(const vp_state *states, int32_t count, int32_t S, int32
         long places = 1;
         for (int j = 0; j < st.dims; ++j) places *= st.sizes[j];
         const long groups = layer_ceil_div(chunks * places, THREADS);
-        if (chunks * places >= (1l << 31) || total + groups * S >= (1l << 31))   // (places are numbered in 32 bits)
+        if (chunks * places >= (1l << 31))   // (numbered in 32 bits within a sentence)
             return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_reorder: state %d is too large", i);
         st.chunks = (unsigned int)chunks;
         st.groups = (unsigned int)groups;
@@ -902,11 +903,14 @@ vp_status vp_beam_reorder(const vp_state *states, int32_t count, const int32_t *
     A.parent = parent;
     if (total == 0 || B == 1) return VP_OK;
     const hipStream_t st = (hipStream_t)hip_stream;
-    const dim3 grid((unsigned int)total);
-    if (B <= 4) hipLaunchKernelGGL((reorder_kernel<4>), grid, dim3(THREADS), 0, st, A);
-    else if (B <= 8) hipLaunchKernelGGL((reorder_kernel<8>), grid, dim3(THREADS), 0, st, A);
-    else if (B <= 16) hipLaunchKernelGGL((reorder_kernel<16>), grid, dim3(THREADS), 0, st, A);
-    else hipLaunchKernelGGL((reorder_kernel<32>), grid, dim3(THREADS), 0, st, A);
+    constexpr long most = LAUNCH_THREADS / THREADS;     // workgroups of a launch
+    for (; A.first < total; A.first += most) {
+        const dim3 grid((unsigned int)std::min<long>(most, total - A.first));
+        if (B <= 4) hipLaunchKernelGGL((reorder_kernel<4>), grid, dim3(THREADS), 0, st, A);
+        else if (B <= 8) hipLaunchKernelGGL((reorder_kernel<8>), grid, dim3(THREADS), 0, st, A);
+        else if (B <= 16) hipLaunchKernelGGL((reorder_kernel<16>), grid, dim3(THREADS), 0, st, A);
+        else hipLaunchKernelGGL((reorder_kernel<32>), grid, dim3(THREADS), 0, st, A);
+    }
     static_assert(VP_MAX_BEAMS <= 32, "rows in registers");
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return (vp_status)vpi_fail(VP_ERR_HIP, "vp_beam_reorder: %s", hipGetErrorString(e));

@@ -184,3 +184,23 @@ def test_embed_grad_of_more_tokens_than_a_launch_has_threads(n, V):
     grad[at] = 0
     for a in range(0, V, 2 ** 28):
         assert not grad[a:a + 2 ** 28].view(torch.int16).any(), a
+
+
+def test_beam_reorder_of_more_pieces_than_a_launch_has_threads():
+    """Bytes whose rows are innermost: a thread for each place of every sentence, in three states one behind the other."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    _room(25)
+    S, B = 4, 2
+    n = S * B
+    parent = torch.tensor([1, 0, 0, 0, 1, 1, -1, 0], dtype=torch.int32, device="cuda")
+    at = torch.tensor([1, 0, 2, 2, 5, 5, 6, 6], device="cuda")
+    step = 2 ** 26
+    line = (torch.arange(step * n, device="cuda") * 7 >> 1).to(torch.uint8).view(step, n)      # (a byte for each place and row)
+    states = [line.repeat(k, 1) for k in (3, 13, 1)]
+    assert sum(t.numel() // B for t in states) > 2 ** 32
+    P.vp_beam_reorder([(t, 1) for t in states], parent, B)
+    want = line[:, at]
+    for t in states:
+        for a in range(0, t.shape[0], step):
+            assert torch.equal(t[a:a + step], want), a
