@@ -409,7 +409,7 @@ vp_status vp_scaled_matmul(const void *packed, int32_t M, int32_t d, const uint8
  *            parent's having or by eos
  * NaN logits count as tokens that are not allowed; a row that holds +inf, or allows nothing, is continued by nothing.
  *   workspace  device, 256-byte aligned, >= vp_beam_select_workspace_bytes(S, B, V)
- * Limits: B <= 32, S * B <= 65536, V <= 2^30. */
+ * Limits: B <= 32, S * B <= 65536, V <= 2^30, and S * B * ceil(V / 8192) < 2^24 (16 bits: / 12288). */
 size_t vp_beam_select_workspace_bytes(int32_t S, int32_t B, int32_t V);
 vp_status vp_beam_select(const void *logits, int32_t type, int64_t stride, const float *scores, int32_t S, int32_t B,
                          int32_t V, const uint32_t *allowed, int64_t allowed_stride, const uint8_t *done, int32_t eos,

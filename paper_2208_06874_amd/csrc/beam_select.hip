@@ -859,7 +859,7 @@ vp_status vp_beam_select(const void *logits, int32_t type, int64_t stride, const
     SelectLayout L;
     select_layout(n, V, B, type, &L);
     if (workspace_bytes < L.total) return (vp_status)vpi_fail(VP_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, L.total);
-    if ((long)n * L.pieces >= (1l << 31)) return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_select: %d rows of %d are too many", n, V);
+    if ((long)n * L.pieces >= (1l << 32) / THREADS) return (vp_status)vpi_fail(VP_ERR_UNSUPPORTED, "vp_beam_select: %d rows of %d are too many", n, V);
     const hipStream_t st = (hipStream_t)hip_stream;
     const SelectArgs A = {logits, (long)stride, (long)allowed_stride, scores, allowed, done, n, V, B, L.pieces, eos,
                           (Piece *)((char *)workspace + L.part), (unsigned long long *)((char *)workspace + L.best),

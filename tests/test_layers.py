@@ -134,3 +134,12 @@ def test_reorder_check_says_what_reorder_would(state, kw, status):
         said = vp.last_error()
         assert vp.lib().vp_beam_reorder(ctypes.byref(state), a["count"], A, a["S"], a["B"], None) == status and vp.last_error() == said
     assert vp.lib().vp_beam_reorder_check(None, 1, 2, 3) == INVALID
+
+
+def test_selection_refuses_more_pieces_than_a_launch_has_threads():
+    """A row is cut into pieces of 8,192 fp32 or 12,288 16-bit values, a workgroup of 256 threads each; a launch has less than 2^32."""
+    most = 1 << 24
+    for code, width in ((0, 12288), (1, 12288), (2, 8192)):
+        for S, V in ((32768, width * (most // 65536) + 1), (8192, 1 << 30)):
+            kw = dict(type=code, S=S, B=2, V=V, stride=V, a_stride=-(-V // 32), ws_bytes=1 << 50)
+            assert _call("vp_beam_select", **kw) == UNSUPPORTED and "too many" in vp.last_error()
