@@ -41,11 +41,11 @@ __device__ inline i32x4 load16_within(const uint8_t *row, int k, int d)
 }
 
 // The weight: [pairs of tiles][column blocks][2 tiles][2 halves][64 lanes][16 bytes], rows and columns past the
-// matrix zero; one thread moves 16 bytes.
+// matrix zero; one thread moves 16 bytes, `first` of which launches before this one have moved.
 __global__ __launch_bounds__(THREADS) void scaled_pack_kernel(const uint8_t *__restrict__ wq, long stride, int M, int d,
-                                                              int blocks, long chunks, i32x4 *__restrict__ packed)
+                                                              int blocks, long first, long chunks, i32x4 *__restrict__ packed)
 {
-    const long id = (long)blockIdx.x * THREADS + threadIdx.x;
+    const long id = first + (long)blockIdx.x * THREADS + threadIdx.x;
     if (id >= chunks) return;
     const int lane = (int)(id & 63), h = (int)(id >> 6) & 1, t = (int)(id >> 7) & 1;
     const long rest = id >> 8;
@@ -432,7 +432,9 @@ vp_status vp_scaled_pack(const uint8_t *wq, int64_t stride, const float *ws, int
     if (packed_bytes < L.total) return (vp_status)vpi_fail(VP_ERR_WORKSPACE, "packed weight of %zu bytes, %zu needed", packed_bytes, L.total);
     const hipStream_t st = (hipStream_t)hip_stream;
     const long chunks = L.row_blocks * BLOCK * L.blocks * (BLOCK / 16);
-    hipLaunchKernelGGL(scaled_pack_kernel, dim3((unsigned int)layer_ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, wq, (long)stride, M, d, (int)L.blocks, chunks, (i32x4 *)((char *)packed + L.w));
+    for (long at = 0; at < chunks; at += LAUNCH_THREADS)
+        hipLaunchKernelGGL(scaled_pack_kernel, dim3((unsigned int)layer_ceil_div(std::min(chunks - at, LAUNCH_THREADS), THREADS)), dim3(THREADS), 0, st, wq, (long)stride, M, d,
+                           (int)L.blocks, at, chunks, (i32x4 *)((char *)packed + L.w));
     hipError_t e = hipMemcpyAsync((char *)packed + L.ws, ws, (size_t)L.row_blocks * L.blocks * 4, hipMemcpyDeviceToDevice, st);
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess) return (vp_status)vpi_fail(VP_ERR_HIP, "vp_scaled_pack: %s", hipGetErrorString(e));

@@ -204,3 +204,22 @@ def test_beam_reorder_of_more_pieces_than_a_launch_has_threads():
     for t in states:
         for a in range(0, t.shape[0], step):
             assert torch.equal(t[a:a + step], want), a
+
+
+def test_scaled_pack_of_more_pieces_than_a_launch_has_threads():
+    """64 GiB and more of weights, a thread for every 16 bytes: the product with rows on both sides of where launches meet."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    M, d = 2 ** 22 + 200, 16384
+    _room(2 * M * d / 1e9)
+    wq = torch.zeros((M, d), dtype=torch.uint8, device="cuda")
+    at = torch.tensor([0, 31, M // 2 - 150, M // 2, 2 ** 21 - 1, 2 ** 21, 2 ** 21 + 77, 2 ** 22 - 1, 2 ** 22, M - 33, M - 1], device="cuda")
+    g = _gen(7)
+    rows = torch.randint(-8, 9, (len(at), d), generator=g, device="cuda").float()
+    wq[at] = rows.to(torch.float8_e4m3fn).view(torch.uint8)
+    packed = P.vp_scaled_pack(wq.view(torch.float8_e4m3fn), torch.ones((-(-M // 128), d // 128), device="cuda"))
+    x = torch.randint(-8, 9, (3, d), generator=g, device="cuda").float()
+    z = P.vp_scaled_matmul(packed, x.to(torch.float8_e4m3fn), torch.ones((3, d // 128), device="cuda"), out_dtype=torch.float32)
+    assert torch.equal(z[:, at].double(), x.double() @ rows.double().t().contiguous())      # (whole numbers: exact)
+    z[:, at] = 0
+    assert not z.any()
