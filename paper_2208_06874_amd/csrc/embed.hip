@@ -235,9 +235,11 @@ struct ItemRoom {
 static_assert(SPAN / 32 == THREADS, "a word of bits for every thread");
 static_assert(SHORT == 16 && TOKENS == 16, "16 lanes for each of a wavefront's four tokens");
 
-// One window of a long list: columns cols .. cols + 512 of the sum over the token's positions in [lo, hi).
+// One window of a long list: columns cols .. cols + 512 of the sum over the token's positions in [lo, hi).  These are found in
+// the list, or among the ids of [lo, hi) where that is shorter: a list of c is cut into c / WINDOW windows, and looking
+// through all of it in each of them goes with the square of c (4,194,304 positions of one token, d = 4: 160 ms, so 3).
 template <typename T, typename G>
-__device__ void grad_item(const T *__restrict__ dout, long stride, long n, int d, float scale, const GradItem it,
+__device__ void grad_item(const T *__restrict__ dout, long stride, const int32_t *__restrict__ ids, long n, int d, float scale, const GradItem it,
                           int item, int cols, const int32_t *__restrict__ list, int count, ItemRoom &R,
                           float *__restrict__ partial, G *__restrict__ grad)
 {
@@ -248,9 +250,11 @@ __device__ void grad_item(const T *__restrict__ dout, long stride, long n, int d
     float acc[1][8] = {};
     if (threadIdx.x == 0) R.n = 0;
     __syncthreads();
-    for (int e = threadIdx.x; e < count; e += THREADS) {
-        const int p = list[e];
-        if (p >= lo && p < hi) {
+    const bool shorter = hi - lo < count;
+    const int entries = shorter ? (int)max(hi - lo, 0l) : count;
+    for (int e = threadIdx.x; e < entries; e += THREADS) {
+        const int p = shorter ? (int)lo + e : list[e];
+        if (shorter ? ids[p] == it.token : p >= lo && p < hi) {
             const int k = atomicAdd(&R.n, 1);
             if (k < SMALL_SORT) R.few[k] = p;
         }
@@ -272,9 +276,14 @@ __device__ void grad_item(const T *__restrict__ dout, long stride, long n, int d
             __syncthreads();
             R.bits[threadIdx.x] = 0;
             __syncthreads();
-            for (int e = threadIdx.x; e < count; e += THREADS) {
-                const int p = list[e];
-                if (p >= at && p < end) atomicOr(&R.bits[(p - at) >> 5], 1u << ((p - at) & 31));
+            if (end - at < count) {
+                for (int e = threadIdx.x; e < (int)(end - at); e += THREADS)
+                    if (ids[at + e] == it.token) atomicOr(&R.bits[e >> 5], 1u << (e & 31));
+            } else {
+                for (int e = threadIdx.x; e < count; e += THREADS) {
+                    const int p = list[e];
+                    if (p >= at && p < end) atomicOr(&R.bits[(p - at) >> 5], 1u << ((p - at) & 31));
+                }
             }
             __syncthreads();
             // every thread lists the positions of its word, behind those of the words before
@@ -320,8 +329,9 @@ __device__ void grad_item(const T *__restrict__ dout, long stride, long n, int d
 // Workgroups 0 .. item_groups - 1 take the windows of long lists, so that these begin first; the others write the
 // rows of TOKENS tokens each from `first` on, a wavefront a row: zeros, or the sum over its list, ordered by counting.
 template <typename T, typename G>
-__global__ __launch_bounds__(THREADS) void grad_rows_kernel(const T *__restrict__ dout, long stride, long n, int V,
-                                                            int d, float scale, const int32_t *__restrict__ count,
+__global__ __launch_bounds__(THREADS) void grad_rows_kernel(const T *__restrict__ dout, long stride,
+                                                            const int32_t *__restrict__ ids, long n, int V, int d,
+                                                            float scale, const int32_t *__restrict__ count,
                                                             const int32_t *__restrict__ start,
                                                             const int32_t *__restrict__ list,
                                                             const GradState *__restrict__ state,
@@ -335,7 +345,7 @@ __global__ __launch_bounds__(THREADS) void grad_rows_kernel(const T *__restrict_
         for (long k = blockIdx.x; k < total; k += item_groups) {
             const int item = (int)(k / cols);
             const GradItem it = items[item];
-            grad_item(dout, stride, n, d, scale, it, item, (int)(k % cols) * ITEM_COLS, list + start[it.token],
+            grad_item(dout, stride, ids, n, d, scale, it, item, (int)(k % cols) * ITEM_COLS, list + start[it.token],
                       count[it.token], R, partial, grad);
         }
         return;
@@ -663,7 +673,7 @@ vp_status vp_embed_grad(const void *dout, int32_t dout_type, int64_t dout_stride
         with_type(dout_type, [&](auto t) {
             with_type(grad_type, [&](auto g) {
                 hipLaunchKernelGGL((grad_rows_kernel<decltype(t), decltype(g)>), grid, dim3(THREADS), 0, st,
-                                   (const decltype(t) *)dout, (long)dout_stride, (long)n, V, d, scale, count, start, list,
+                                   (const decltype(t) *)dout, (long)dout_stride, ids, (long)n, V, d, scale, count, start, list,
                                    state, items, windows, at * TOKENS, partial, (decltype(g) *)grad);
             });
         });

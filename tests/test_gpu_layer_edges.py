@@ -223,3 +223,70 @@ def test_scaled_pack_of_more_pieces_than_a_launch_has_threads():
     assert torch.equal(z[:, at].double(), x.double() @ rows.double().t().contiguous())      # (whole numbers: exact)
     z[:, at] = 0
     assert not z.any()
+
+
+# ---------------------------------------------------------------- lists of the embedding's gradient
+def _clustered(n, V, where):
+    """Tokens from 20 on all over, none of them often; `where`: token -> the positions that it has."""
+    torch = _torch()
+    ids = 20 + (torch.arange(n, device="cuda") * 7919 % (V - 20)).to(torch.int32)
+    for token, at in where.items():
+        ids[at] = token
+    return ids
+
+
+@pytest.mark.parametrize("kind", ["lengths", "a run in a wide window", "a run in narrow windows", "a long run in a wide window", "every second", "two tokens"])
+@pytest.mark.parametrize("d,dout,grad", [(24, "float16", "float32"), (520, "bfloat16", "bfloat16"), (1031, "float32", "float32")])
+def test_embed_grad_lists(kind, d, dout, grad):
+    """Lists whose positions are found and ordered in each of the ways there are."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    r = lambda a, b, s=1: torch.arange(a, b, s, device="cuda")  # noqa: E731
+    n, V, where = {
+        # at the borders of one wavefront's lists, of one window, of two
+        "lengths": (9000, 4000, {k: r(100 * k, 100 * k + 99 * (c - 1) + 1, 99) % 9000 if c < 90 else r(5000 + k, 5000 + k + 13 * c, 13) % 9000
+                                 for k, c in enumerate((1, 15, 16, 17, 127, 128, 129, 256, 257))}),
+        # 300 positions, cut into three windows of 13,334, all in one: more than are ordered by comparing, twice 8,192 positions as bits
+        "a run in a wide window": (40000, 30000, {3: r(20000, 20300)}),
+        # 10,000 in 79 windows of 2,532 positions: fewer than the list has entries
+        "a run in narrow windows": (200000, 30000, {3: r(50000, 60000)}),
+        # 9,000 in 71 windows of 14,085, nearly all in two of them
+        "a long run in a wide window": (1000000, 30000, {3: r(500000, 509000)}),
+        "every second": (30000, 5000, {1: r(0, 30000, 2)}),
+        "two tokens": (20001, 30, {0: r(0, 20001), 5: r(3, 20001, 17)})}[kind]
+    if kind == "a long run in a wide window" and d > 600:
+        n, where = 600000, {3: r(300000, 309000)}
+    ids = _clustered(n, V, where)
+    x = _randn(_gen(d), (n, d), dout)
+    got = P.vp_embed_grad(x, ids, V, scale=0.5, grad_dtype=_t(grad))
+    at = ids.long()
+    count = torch.bincount(at, minlength=V).double()
+    assert kind != "lengths" or count[:9].tolist() == [1, 15, 16, 17, 127, 128, 129, 256, 257]
+    want, size = (torch.zeros((V, d), dtype=torch.float64, device="cuda") for _ in range(2))
+    for a in range(0, n, 100000):
+        want.index_add_(0, at[a:a + 100000], x[a:a + 100000].double() * 0.5)
+        size.index_add_(0, at[a:a + 100000], x[a:a + 100000].double().abs() * 0.5)
+    _within(got, want, size * (count[:, None] + 1) * U + want.abs() * _half_step(grad) * 1.001 + LEAST[grad])
+    assert torch.equal(got, P.vp_embed_grad(x, ids, V, scale=0.5, grad_dtype=_t(grad)))
+
+
+def test_embed_grad_of_one_token_goes_with_its_positions():
+    """Four times the positions of one token take about four times as long, not sixteen."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+
+    def least(n):
+        ids, x, best = torch.full((n,), 7, device="cuda", dtype=torch.int32), torch.ones((n, 4), device="cuda", dtype=torch.float16), math.inf
+        out = P.vp_embed_grad(x, ids, 100)
+        assert float(out[7, 0]) == n and float(out.sum()) == 4 * n      # (whole numbers below 2^24: exact)
+        for _ in range(4):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            P.vp_embed_grad(x, ids, 100)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best
+
+    few, many = least(2 ** 20), least(2 ** 22)
+    assert many < 9 * few, "%.3f and %.3f ms" % (few, many)
