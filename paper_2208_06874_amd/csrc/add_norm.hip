@@ -299,6 +299,9 @@ vp_status vp_add_norm(const void *x, int64_t x_stride, const void *residual, int
     if ((q == nullptr) != (scales == nullptr)) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_add_norm: q and scales go together");
     if (n == 0) return VP_OK;
     if (!x || !weight) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_add_norm: null pointer argument");
+    // (a row's sum would lie on another row's elements)
+    if (n > 1 && sum && ((sum == x && x_stride != d) || (sum == residual && residual_stride != d)))
+        return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_add_norm: sum over rows that are not contiguous");
     const size_t a = type_size(type);
     if (!layer_aligned(x, a) || !layer_aligned(residual, a) || !layer_aligned(sum, a) || !layer_aligned(weight, type_size(weight_type)) ||
         (norm && !layer_aligned(norm, type_size(norm_type))) || !layer_aligned(q, 8) || !layer_aligned(scales, 4) || !layer_aligned(rstd, 4))

@@ -143,3 +143,8 @@ def test_selection_refuses_more_pieces_than_a_launch_has_threads():
         for S, V in ((32768, width * (most // 65536) + 1), (8192, 1 << 30)):
             kw = dict(type=code, S=S, B=2, V=V, stride=V, a_stride=-(-V // 32), ws_bytes=1 << 50)
             assert _call("vp_beam_select", **kw) == UNSUPPORTED and "too many" in vp.last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(x_stride=65), dict(r_stride=65), dict(x_stride=1000, residual=A + 0x100000), dict(r_stride=64 + 8, x=A + 0x100000)])
+def test_norm_refuses_a_sum_over_rows_that_are_apart(kw):
+    assert _call("vp_add_norm", **kw) == INVALID and "contiguous" in vp.last_error()
