@@ -794,7 +794,10 @@ vp_status reorder_states(const vp_state *states, int32_t count, int32_t S, int32
         int64_t reach = 1;
         for (int j = 0; j < kept; ++j) {
             if (in.strides[order[j]] < reach) return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d overlaps itself", i);
-            reach = (in.sizes[order[j]] - 1) * in.strides[order[j]] + reach;
+            // (so that no product below overflows)
+            int64_t span;
+            if (__builtin_mul_overflow(in.sizes[order[j]] - 1, in.strides[order[j]], &span) || __builtin_add_overflow(span, reach, &reach) || reach > (1ll << 48))
+                return (vp_status)vpi_fail(VP_ERR_INVALID_ARG, "vp_beam_reorder: state %d reaches past any memory", i);
         }
         StateArgs &st = A->state[A->states];
         st.base = (char *)in.data;

@@ -148,3 +148,10 @@ def test_selection_refuses_more_pieces_than_a_launch_has_threads():
 @pytest.mark.parametrize("kw", [dict(x_stride=65), dict(r_stride=65), dict(x_stride=1000, residual=A + 0x100000), dict(r_stride=64 + 8, x=A + 0x100000)])
 def test_norm_refuses_a_sum_over_rows_that_are_apart(kw):
     assert _call("vp_add_norm", **kw) == INVALID and "contiguous" in vp.last_error()
+
+
+@pytest.mark.parametrize("state", [_state([2, 1 << 61], [1 << 61, 1], elem=8), _state([2, 1 << 62], [1 << 62, 1], elem=4), _state([2, 3, 1 << 40], [1, 1 << 62, 2]),
+                                   _state([2, 1 << 49], [1, 2], elem=1)])
+def test_reorder_refuses_sizes_past_any_memory(state):
+    """Their products leave 64 bits: nothing may be made of what is left of them."""
+    assert vp.lib().vp_beam_reorder_check(ctypes.byref(state), 1, 1, 2) == INVALID and "memory" in vp.last_error()
