@@ -380,9 +380,11 @@ vp_status vp_add_norm_grad(const void *dnorm, int64_t dnorm_stride, const void *
 
 /* 8-bit product with scales of blocks of 128:
  *   out[i, m] = sum over column blocks b of xs[i, b] * ws[m / 128, b] * (sum over k in b of xq[i, k] * wq[m, k]) + bias[m]
- * rounded once.  The blocks are added in 32 bits.  Within a block fp32 outputs are summed in 32 bits as well; for
- * fp16 and bf16 outputs the 8-bit matrix instructions sum, which cut off what lies about 2^-12 below a block's largest
- * product (1.4e-5 of the result on normal data, where rounding to fp16 costs 2.1e-4).  The weight is laid out once:
+ * rounded once.  The blocks are added in 32 bits.  Within a block fp32 outputs are summed in 32 bits as well.  For fp16 and
+ * bf16 outputs the 8-bit matrix instructions sum: of every eight neighbouring columns' products each is cut to a multiple of
+ * 2^-13 of the largest one's binade, so that less than 7 * 2^-13 of the largest is lost; sums of eight are added in 32 bits.
+ * (1.4e-5 of the result on normal data, 6e-5 where one column of a block is 20 times and more the others; rounding to fp16
+ * costs 2.1e-4.)  The weight is laid out once:
  *   wq      device, e4m3 bytes [M, d];  ws  device, fp32 [ceil(M / 128), ceil(d / 128)]
  *   packed  device, 256-byte aligned, >= vp_scaled_pack_bytes(M, d); holds wq and ws from then on
  * and a call takes
