@@ -4,7 +4,7 @@ import math
 
 import pytest
 
-from tests.test_gpu_layers import LEAST, U, _bits, _gen, _half_step, _quantized, _randn, _same_selection, _select, _t, _torch, _within
+from tests.test_gpu_layers import LEAST, U, _bits, _gen, _half_step, _lists, _quantized, _randn, _same_selection, _select, _t, _torch, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -346,3 +346,142 @@ def test_scaled_matmul_of_columns_of_different_sizes(n, M, d, kind, out):
         past = z.isinf() & (z * want > 0) & (want.abs() + bound > most)         # (what is past the type's range becomes infinite)
         assert past.all() or not (want.abs() - bound > most * (1 + _half_step(out)))[~past].any()
         _within(torch.where(past, want, z), want, bound)
+
+
+# ---------------------------------------------------------------- graphs, streams, long offsets on the paths of many rows
+def test_embed_grad_through_lists_replayed_from_a_graph():
+    """More than 1,024 positions: counters, cursors and lists in the workspace are cleared by every replay."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    g = _gen(31)
+    n, V, d = 9000, 700, 130
+    x, ids = _randn(g, (n, d), "bfloat16"), _lists("mixed", n, V, g)
+    P.vp_embed_grad(x, ids, V, padding_id=1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = P.vp_embed_grad(x, ids, V, padding_id=1)
+    for rep in range(6):
+        ids.copy_(_lists(("mixed", "one", "few", "runs")[rep % 4], n, V, g))
+        x.copy_(_randn(g, (n, d), "bfloat16"))
+        want = P.vp_embed_grad(x, ids, V, padding_id=1).clone()
+        torch.cuda.synchronize()
+        print("replay", rep, flush=True)
+        held.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, want)
+
+
+@pytest.mark.parametrize("n,M,d,out", [(600, 4000, 300, "float16"), (600, 4000, 300, "float32"), (130, 70000, 256, "bfloat16"), (40, 5000, 700, "float16")])
+def test_scaled_matmul_of_many_rows_replayed_from_a_graph(n, M, d, out):
+    """The rows are laid out in the workspace first."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    g = _gen(n)
+    (xq, xs), (wq, ws) = _quantized(_randn(g, (n, d), "float32"), 1), _quantized(_randn(g, (M, d), "float32"), 128)
+    packed, b = P.vp_scaled_pack(wq, ws), _randn(g, (M,), "float32")
+    P.vp_scaled_matmul(packed, xq, xs, bias=b, out_dtype=_t(out))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = P.vp_scaled_matmul(packed, xq, xs, bias=b, out_dtype=_t(out))
+    for rep in range(4):
+        q, s = _quantized(_randn(g, (n, d), "float32"), 1)
+        xq.copy_(q), xs.copy_(s)
+        want = P.vp_scaled_matmul(packed, xq, xs, bias=b, out_dtype=_t(out)).clone()
+        torch.cuda.synchronize()
+        print("replay", rep, flush=True)
+        held.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, want)
+
+
+def test_selection_of_many_rows_replayed_from_a_graph():
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    g = _gen(33)
+    S, B, V = 24, 8, 30011
+    n = S * B
+    z, scores = _randn(g, (n, V), "float16", 2.0), -torch.rand(n, generator=g, device="cuda")
+    bits, done = _bits(g, n, V, 0.8), (torch.rand(n, generator=g, device="cuda") < 0.2).to(torch.uint8)
+    f = lambda: P.vp_beam_select(z, scores, B, allowed=bits, done=done, eos=2)  # noqa: E731
+    f()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = f()
+    for rep in range(4):
+        z.copy_(torch.zeros_like(z) if rep == 2 else _randn(g, (n, V), "float16", 2.0))      # (ties of whole rows once)
+        scores.copy_(-torch.rand(n, generator=g, device="cuda"))
+        want = [t.clone() for t in f()]
+        torch.cuda.synchronize()
+        print("replay", rep, flush=True)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
+def test_paths_of_many_rows_on_other_streams():
+    """Lists of the embedding's gradient and rows of the product, each call with a workspace on its own stream, interleaved."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    g = _gen(34)
+    n, V, d, M = 9000, 900, 200, 3000
+    x, ids = _randn(g, (n, d), "float16"), _lists("mixed", n, V, g)
+    (xq, xs), (wq, ws) = _quantized(_randn(g, (n, d), "float32"), 1), _quantized(_randn(g, (M, d), "float32"), 128)
+    packed = P.vp_scaled_pack(wq, ws)
+    want = P.vp_embed_grad(x, ids, V), P.vp_scaled_matmul(packed, xq, xs)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for rep in range(9):
+        st = streams[rep % 3]
+        if rep % 2:
+            got.append((P.vp_embed_grad(x, ids, V, stream=st), P.vp_scaled_matmul(packed, xq, xs, stream=st)))
+        else:
+            with torch.cuda.stream(st):
+                got.append((P.vp_embed_grad(x, ids, V), P.vp_scaled_matmul(packed, xq, xs)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, want[0]) and torch.equal(b, want[1]) for a, b in got)
+
+
+def test_embed_grad_through_lists_past_32_bits():
+    """Rows of the gradient, and of what it is made of, past 2^31 elements."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    _room(16)
+    d, V, n = 4096, 600000, 530000
+    tokens = torch.tensor([0, V - 1, V // 2, 524287, 524288, 524289], dtype=torch.int32, device="cuda")
+    ids = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    at = torch.tensor([0, n - 1, 524288, 524287, 7, 524290], device="cuda")
+    ids[at] = tokens
+    ids[n - 500:n - 1] = V - 1                            # (a list of several windows)
+    x = torch.zeros((n, d), dtype=torch.float16, device="cuda")
+    rows = torch.randint(-8, 9, (6, d), generator=_gen(1), device="cuda").half()
+    x[at] = rows
+    x[n - 500:n - 1, ::3] = 1.0
+    grad = torch.full((V, d), math.nan, dtype=torch.float16, device="cuda")
+    P.vp_embed_grad(x, ids, V, out=grad)
+    want = rows.clone()
+    want[1, ::3] += 499
+    assert torch.equal(grad[tokens.long()], want)
+    grad[tokens.long()] = 0
+    assert not grad.view(torch.int16).any()
+
+
+def test_logits_past_32_bits_to_their_own_rounding():
+    """fp32 logits are sums in 32 bits: no more than those roundings, past 2^31 elements."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    _room(12)
+    n, M, d = 2000, 1200000, 32
+    g = _gen(2)
+    (xq, xs), (wq, ws) = _quantized(_randn(g, (n, d), "float32"), 1), _quantized(_randn(g, (M, d), "float32"), 128)
+    z = P.vp_scaled_matmul(P.vp_scaled_pack(wq, ws), xq, xs, out_dtype=torch.float32)
+    at = torch.tensor([0, 1, 999, 1789, 1790, 1999], device="cuda")
+    x = xq[at].float().double() * xs[at].double()
+    w = (wq.float().double() * ws.double().repeat_interleave(128, 0)[:M]).t().contiguous()
+    want = x @ w
+    _within(z[at], want, (x.abs() @ w.abs()) * (32 * 2 + 5) * U + want.abs() * U)       # 32 additions that may cut off, the scales
