@@ -327,10 +327,10 @@ vp_status vp_beam_step(const int32_t *cand_ids, const float *cand_logp, const fl
                        void *hip_stream);
 
 /* ---- Layers next to the projection: embedding, norm, 8-bit product, beam search over whole rows ----
- * All of them only enqueue kernels on hip_stream, allocate nothing and may be captured into a graph.  Rows have
- * contiguous elements; a stride counts elements from row to row (>= the row's length) and any address that is a
- * multiple of one element will do.  Outputs without a stride are contiguous.  Equal inputs give bit-identical
- * outputs. */
+ * All of them only enqueue work on hip_stream (kernels; vp_scaled_pack also a copy between device buffers), allocate
+ * nothing and may be captured into a graph.  Rows have contiguous elements; a stride counts elements from row to row (>= the
+ * row's length) and any address that is a multiple of one element will do.  Outputs without a stride are contiguous.
+ * Equal inputs give bit-identical outputs. */
 typedef enum { VP_F16 = 0, VP_BF16 = 1, VP_F32 = 2 } vp_type;
 #define VP_MAX_BEAMS 32
 #define VP_SCALED_MAX_DIM 16384
@@ -403,7 +403,7 @@ vp_status vp_scaled_matmul(const void *packed, int32_t M, int32_t d, const uint8
 /* Beam search over whole rows of logits: for each of S sentences the B best of
  *   total(b, t) = scores[b] + logits[b, t] - log sum over allowed t' of exp(logits[b, t'])
  * in the order total descending, then b, then t.  Row s * B + b belongs to hypothesis b of sentence s.
- *   logits   device, type [S * B, V];  scores  device, fp32 [S * B] (-inf: dead, continued by nothing)
+ *   logits   device, type [S * B, V];  scores  device, fp32 [S * B] (-inf or NaN: dead, continued by nothing)
  *   allowed  device, bit t % 32 of word t / 32 of a row set: t may follow; allowed_stride words from row to row;
  *            NULL: every token may
  *   done     device, uint8 [S * B], or NULL: a hypothesis that has ended goes on with eos at its own score only
