@@ -225,6 +225,7 @@ __global__ __launch_bounds__(THREADS, 2) void scaled_gemm_kernel(const MatmulArg
     __shared__ float scales0[TN * 16], scales1[TN * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // neighbouring tiles on one XCD, whose L2 then serves them the same rows and weights: GROUP weight tiles x all row tiles
+    // (4,096 rows on 250,000 x 1,536: 1,544 us, with four 1,566, five times in turn)
     constexpr int GROUP = 8;
     const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if (t >= m_tiles * n_tiles) return;
@@ -500,22 +501,32 @@ vp_status vp_scaled_matmul(const void *packed, int32_t M, int32_t d, const uint8
     typedef std::integral_constant<int, 2> Two;
     typedef std::integral_constant<int, 4> Four;
     typedef std::integral_constant<int, 8> Eight;
+    // (The figures below are us of the whole call in fp16 unless said otherwise, rows on M x d.)
     // One row tile, or so few tiles of 32 x 16 that a workgroup's walk along the columns would be most of the time: the
-    // columns split among wavefronts.  us, split against tiles of 128 x 64: 20 rows on 1,000 x 4,096 6.0, 18.9; 1,000 on
-    // 1,000 x 1,000 7.9, 10.2; beyond, 40 on 20,000 x 1,500 14.3, 11.7; 64 on 32,000 x 1,024 16.1, 11.0.
+    // columns split among wavefronts.  Split against tiles of 128 x 64: 20 on 1,000 x 4,096 6.1, 19.3; at the border 32 on
+    // 24,000 x 1,024 7.9, 8.9 and on 25,000 9.4, 9.1; it lies higher for fewer columns (1,000 on 1,000 x 1,000, 2,016 tiles, 7.9, 9.7;
+    // 32 on 40,000 x 512, 2,500, 6.7, 7.8) and lower for more (32 on 20,000 x 4,096, 1,250, 23.2, 21.6); far beyond, 64 on 32,000 x
+    // 1,024 16.1, 10.4.
     const long split_tiles = layer_ceil_div(M, 32) * tiles;
     if (tiles == 1 || split_tiles <= 1536) {
-        // two row tiles to a workgroup read the weight once for both, and halve the workgroups (24 rows on 8,000 x 1,000 4.4
-        // against 5.4; 64 on 1,000 x 4,096 10.0 against 6.8)
-        if (tiles == 1 || split_tiles <= 256 || (tiles > 2 && split_tiles <= 640)) few(One{});
+        // Two row tiles to a workgroup read the weight once for both, and halve the workgroups.  One tile against two: up to
+        // 256 workgroups, one for each compute unit, 32 on 4,000 x 1,024 3.8, 4.5; 64 on 1,000 x 4,096 6.2, 9.5; up to 640 24 on
+        // 8,000 x 1,000 4.5, 4.5; 48 on 6,700 x 512 4.0, 4.2; 128 on 2,500 x 1,024 5.6, 6.2 (x 4,096 16.9, 16.6); beyond, 48 on 9,000 x 1,024
+        // still 6.6, 7.1, but 32 on 20,000 x 1,024 9.1, 7.7; 128 on 6,000 x 4,096 26.8, 23.1.
+        if (tiles == 1 || split_tiles <= 640) few(One{});
         else few(Two{});
     } else if (out_type == VP_F32) {
-        // (widened weights take twice the registers)
+        // (Widened weights take twice the registers: tiles of half the height.)  From enough tiles of 128 x 128 for every compute
+        // unit's two workgroups on these, against tiles of 128 x 64: 4,096 on 50,000 x 1,536 619, 647; 2,000 on 10,000 x 2,000 86, 92;
+        // but 300 on 250,000 x 1,024 203, 185; just below the border 1,000 on 8,000 x 1,024 (504) 23.4, 25.0, just beyond, where a second
+        // round begins, on 8,400 (528) 31.1, 28.2.
         if (layer_ceil_div(M, 128) * layer_ceil_div(tiles, 8) >= 512) many(Two{}, Eight{}, float{});
         else many(Two{}, Four{}, float{});
     } else if (tiles > 2 && layer_ceil_div(M, 256) * layer_ceil_div(tiles, 8) >= 512) {
-        // enough tiles of 256 x 128 for every compute unit's two workgroups: 100 rows on 250,000 x 1,024 62 against 72 in tiles
-        // of 128 x 64, 2,000 on 10,000 x 2,000 52 against 59; with fewer, 128 on 32,000 x 512 11.2 against 9.3
+        // Enough tiles of 256 x 128 for every compute unit's two workgroups.  Against tiles of 128 x 64: 2,000 on 10,000 x 2,000
+        // 50, 55; 100 on 250,000 x 512 34.4, 35.1, x 1,024 52, 53, x 2,048 113, 129; just below the border 128 on 120,000 x 2,048 (469) 47, 51,
+        // just beyond, where a second round begins, on 132,000 (516) 65, 59; far below 128 on 32,000 x 512 11.2, 8.3.  Two row tiles
+        // leave three quarters of one empty: 32 on 250,000 x 512 30, 28.
         if (out_type == VP_F16) many(Four{}, Eight{}, Half{});
         else many(Four{}, Eight{}, Bf16{});
     } else {
