@@ -125,6 +125,13 @@ __global__ __launch_bounds__(64 * waves_of(W)) void add_norm_kernel(const NormAr
     float y[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) y[j] = f[j] * rstd * w[j];
+    // past d no part in the scale and bytes of zero, though rstd or the scale may be no number or infinite (the bytes without a
+    // branch: with one around what was packed, 16,384 x 1,536 bf16 took 33.3 us instead of 33.0)
+    const int left = d - c;
+    if (left < 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = j < left ? y[j] : 0.f;
+    }
     if (A.norm) {
         const size_t at = (size_t)row * d;
         if (A.norm_type == VP_F16) put_within((Half *)A.norm + at, c, d, y, A.stream);
@@ -132,12 +139,6 @@ __global__ __launch_bounds__(64 * waves_of(W)) void add_norm_kernel(const NormAr
         else put_within((float *)A.norm + at, c, d, y, A.stream);
     }
     if (A.q) {
-        // past d no part in the scale and bytes of zero, though rstd or the scale may be no number or infinite
-        const int left = d - c;
-        if (left < 8) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = j < left ? y[j] : 0.f;
-        }
         unsigned int most = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(y[j]) & 0x7fffffffu);
@@ -148,11 +149,10 @@ __global__ __launch_bounds__(64 * waves_of(W)) void add_norm_kernel(const NormAr
         for (int h = 0; h < 2; ++h) {
             float p[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) p[j] = y[h * 4 + j] / scale;
+            for (int j = 0; j < 4; ++j) p[j] = h * 4 + j < left ? y[h * 4 + j] / scale : 0.f;
             int word = __builtin_amdgcn_cvt_pk_fp8_f32(p[0], p[1], 0, false);
             packed[h] = (unsigned int)__builtin_amdgcn_cvt_pk_fp8_f32(p[2], p[3], word, true);
         }
-        if (left < 8) packed = __builtin_bit_cast(u32x2, __builtin_bit_cast(unsigned long long, packed) & ((1ull << 8 * max(left, 0)) - 1ull));
         if (c < blocks * BLOCK) {
             u32x2 *const to = (u32x2 *)(A.q + (size_t)row * blocks * BLOCK + c);
             if (A.stream) VP_STREAM_STORE(to, packed);
