@@ -485,3 +485,40 @@ def test_logits_past_32_bits_to_their_own_rounding():
     w = (wq.float().double() * ws.double().repeat_interleave(128, 0)[:M]).t().contiguous()
     want = x @ w
     _within(z[at], want, (x.abs() @ w.abs()) * (32 * 2 + 5) * U + want.abs() * U)       # 32 additions that may cut off, the scales
+
+
+# ---------------------------------------------------------------- norm, to the sums as they are made
+@pytest.mark.parametrize("n,d,kind", [(300, 500, "float32"), (300, 512, "bfloat16"), (200, 1024, "float32"), (200, 1500, "float32"), (100, 2049, "float16"), (100, 4096, "float32"), (7, 3600, "bfloat16")])
+def test_add_norm_to_its_own_roundings(n, d, kind):
+    """A lane adds eight squares, six joins the lanes of a wavefront, and the row's wavefronts follow one by one."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    g = _gen(n + d)
+    x, r, w = _randn(g, (n, d), kind), _randn(g, (n, d), kind), (1 + _randn(g, (d,), "float32", 0.1))
+    eps = float(torch.tensor(1e-6))
+    got = P.vp_add_norm(x, w, residual=r, eps=eps, norm_dtype=torch.float32, rstd=True)
+    s = (x.float() + r.float()).to(x.dtype)
+    assert torch.equal(got.sum, s)
+    f = s.double()
+    rstd = 1 / torch.sqrt(f.square().mean(1) + eps)
+    rel = ((8 + 6 + -(-d // 512) - 1) / 2 + 4) * U       # (the root halves; mean, eps, root, quotient)
+    _within(got.rstd, rstd, rstd * rel)
+    y = f * rstd[:, None] * w.double()
+    _within(got.norm, y, y.abs() * (rel + 2 * U))
+
+
+@pytest.mark.parametrize("n,d", [(3, 100), (4097, 500), (9000, 512), (5000, 1000), (2100, 1024), (5000, 1500), (1025, 4096), (3100, 2050)])
+def test_add_norm_grad_of_the_weight_to_its_own_roundings(n, d):
+    """Up to 1,024 workgroups of four, two or one rows (rows of up to 512, of up to 1,024, wider): the rows of a wavefront, the rows of
+    a workgroup, the workgroups in 32 strands, and five joins of these."""
+    torch = _torch()
+    import paper_2208_06874_amd as P
+    g = _gen(n + d)
+    s, dn, w = _randn(g, (n, d), "float32", 3.0), _randn(g, (n, d), "float32"), _randn(g, (d,), "float32")
+    r = torch.rsqrt(s.double().square().mean(1) + 1e-6).float()
+    _, dw = P.vp_add_norm_grad(dn, s, w, r)
+    together = 4 if d <= 512 else 2 if d <= 1024 else 1
+    groups = min(1024, -(-n // together))
+    chain = -(-n // (groups * together)) + (together - 1) + -(-groups // 32) + 5 + 1      # (and the rounding of s * rstd)
+    terms = dn.double() * s.double() * r.double()[:, None]
+    _within(dw, terms.sum(0), terms.abs().sum(0) * chain * U)
